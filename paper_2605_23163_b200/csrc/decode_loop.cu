@@ -110,13 +110,15 @@ fdd_status fdd_decode_block(fdd_ctx* ctx, fdd_forkset* const* sets, int n_sets, 
         return FDD_ERR_INVALID_ARG;
     }
     int forks = 0;
-    for (int s = 0; s < n_sets; ++s) {
+    for (int s = 0; s < n_sets; ++s)
         if (!sets[s]) {
             ctx->last_error = "fdd_decode_block: a fork set is NULL";
             return FDD_ERR_INVALID_ARG;
         }
-        forks += sets[s]->n_forks;
-    }
+    // (the attention would refuse these sets, side by side only behind the first unmasking)
+    const fdd_status usable = check_loop_sets(ctx, sets, n_sets);
+    if (usable != FDD_OK) return usable;
+    for (int s = 0; s < n_sets; ++s) forks += sets[s]->n_forks;
     if (forks > ctx->cfg.max_forks) {
         ctx->last_error = "fdd_decode_block: more rollouts than the context was created for";
         return FDD_ERR_CAPACITY;

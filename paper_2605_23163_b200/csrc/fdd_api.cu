@@ -222,6 +222,12 @@ fdd_status quantize_layer(fdd_ctx* ctx, fdd_forkset* const* sets, int n_sets, in
 
 }  // namespace
 
+fdd_status check_loop_sets(fdd_ctx* ctx, fdd_forkset* const* sets, int n_sets) {
+    for (int s = 0; s < n_sets; ++s)
+        if (!set_alive(ctx, sets[s])) return fail(ctx, FDD_ERR_STATE, "fork set %d is not a live set of this context", s);
+    return check_one_type(ctx, sets, n_sets);
+}
+
 // Layers of a step are calls of their own to the caller, but their inputs are all in place before the first of them
 // (fdd_decode_block), so they go to the kernel like the scenes of one call: equal ranges over the tile steps of up to
 // kTcMaxSets (scene, layer) pairs fill the chip, where a layer of a few rollouts alone is cut into many pieces that have

@@ -267,6 +267,8 @@ struct ScoreArgs {
 cudaError_t launch_score(ScoreArgs a, int logits_dtype, int sm_count, cudaStream_t st);
 static_assert(sizeof(CommitArgs) <= 4096, "the arguments of an append launch");
 cudaError_t launch_kv_commit(const CommitArgs& a, int sm_count, cudaStream_t st);
+// The sets of a block loop are live and hold their prefixes in one type.
+fdd_status check_loop_sets(fdd_ctx* ctx, fdd_forkset* const* sets, int n_sets);
 // fdd_block_attn_gated and fdd_kv_commit (to_prefix: fdd_prefix_extend) of layers [first_layer, first_layer + n_layers);
 // the pointer arrays have one entry per layer.  beside: other kernels run at the same time.
 fdd_status block_attn_layers(fdd_ctx* ctx, fdd_forkset* const* sets, int n_sets, int first_layer, int n_layers,

@@ -1,0 +1,102 @@
+"""What the library's host side checks and does before a launch, on a CPU: its objects are linked with a stand-in for the CUDA
+runtime (fake_cudart.cpp) that counts launches instead of making them."""
+import ctypes
+import os
+import subprocess
+
+import numpy as np
+import pytest
+
+from paper_2605_23163_b200 import build, fdd
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+
+
+@pytest.fixture(scope="module")
+def host_library(tmp_path_factory):
+    build.build_library()
+    objects = [os.path.join(build.OBJ, os.path.basename(s)[:-3] + ".o") for s in build.sources()]
+    if not all(os.path.exists(o) for o in objects):
+        build.build_library(force=True)
+    out = str(tmp_path_factory.mktemp("host") / "libfdd_host.so")
+    cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
+    cmd = ["g++", "-shared", "-fPIC", "-std=c++17", "-O1", "-I", os.path.join(cuda, "include"), os.path.join(HERE, "fake_cudart.cpp")] + objects + \
+          ["-Wl,-Bsymbolic", "-o", out]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    assert res.returncode == 0, res.stderr
+    return out
+
+
+@pytest.fixture
+def host(host_library, monkeypatch):
+    monkeypatch.setattr(fdd, "LIB_PATH", host_library)
+    monkeypatch.setattr(fdd, "_lib_handle", None)
+    L = fdd.lib()
+    L.fake_launches.restype = ctypes.c_ulonglong
+    L.fake_set_device(0)
+    yield L
+    L.fake_set_device(0)
+
+
+class Buffers:
+    """Host arrays whose addresses stand for device memory, 256-byte aligned, zeroed."""
+
+    def __init__(self):
+        self.kept = []
+
+    def __call__(self, n):
+        raw = np.zeros(n + 256, dtype=np.uint8)
+        self.kept.append(raw)
+        return raw.ctypes.data + (-raw.ctypes.data) % 256
+
+
+HQ, HKV, DIM, BLOCK, VOCAB, CAP = 4, 2, 64, 16, 64, 256
+GROUPS = CAP // 64
+
+
+@pytest.fixture
+def ctx(host):
+    c = fdd.fdd_create(HQ, HKV, DIM, VOCAB, 1, 0, BLOCK, 8, fdd.FDD_LOGITS_F32)
+    yield c
+    fdd.fdd_destroy(c)
+
+
+@pytest.fixture
+def buf():
+    return Buffers()
+
+
+def _quantized(ctx, buf, n=1, length=64, cap=CAP, k=None, v=None, ek=None, ev=None):
+    k, v = (p or buf(HKV * CAP * DIM) for p in (k, v))
+    ek, ev = (p or buf(HKV * GROUPS) for p in (ek, ev))
+    return fdd.fdd_fork_quantized(ctx, [k], [v], [ek], [ev], None, length, cap, n, range(n), [None], [None], 0)
+
+
+def _plain(ctx, buf, n=1, length=64):
+    return fdd.fdd_fork(ctx, [buf(2 * HKV * CAP * DIM)], [buf(2 * HKV * CAP * DIM)], None, length, CAP, n, range(n), [None], [None], 0)
+
+
+def _refused(status, fn, *args, **kw):
+    with pytest.raises(fdd.FddError) as e:
+        fn(*args, **kw)
+    assert e.value.status == status, e.value
+
+
+@pytest.mark.parametrize("first", ["bits8", "bf16"])
+@pytest.mark.parametrize("callback", [False, True])
+def test_a_block_loop_over_prefixes_of_both_types_is_refused_before_anything_happens(host, ctx, buf, first, callback):
+    sets = [_quantized(ctx, buf), _plain(ctx, buf)]
+    if first == "bf16":
+        sets.reverse()
+    rows = 2 * BLOCK
+    q, k, v, out = buf(rows * HQ * DIM * 2), buf(rows * HKV * DIM * 2), buf(rows * HKV * DIM * 2), buf(rows * HQ * DIM * 2)
+    called = []
+    step_fn = ctypes.CFUNCTYPE(None, ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p)(lambda user, t, stream: called.append(t))
+    steps, left = ctypes.c_int(), ctypes.c_int()
+    launched = host.fake_launches()
+    status = host.fdd_decode_block(
+        ctx, fdd.ptr_array(sets), 2, 1, 4, 1, *(fdd.ptr_array([x]) for x in (q, k, v, out, buf(rows * VOCAB * 4))), buf(rows * 4), buf(rows),
+        fdd.i32_array([BLOCK, BLOCK]), 0.125, 0, 0.9, 1.0, 0, 0, buf(8), buf(8), ctypes.byref(steps), ctypes.byref(left),
+        step_fn if callback else None, None, None)
+    assert status == fdd.FDD_ERR_STATE
+    assert host.fake_launches() == launched and not called
