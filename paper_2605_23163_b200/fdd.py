@@ -130,7 +130,12 @@ def _ptr(t):
 
 def _rows_ptr(t, row_stride):
     """Device address of rows [n][...] that lie `row_stride` entries apart, each contiguous (or as _ptr)."""
-    if t is None or isinstance(t, (int, ctypes.c_void_p)) or t.is_contiguous():
+    if t is None or isinstance(t, (int, ctypes.c_void_p)):
+        return _ptr(t)
+    if t.is_contiguous():
+        # (rows may be counted by several dimensions; what fits into one pitch is one row)
+        if t.numel() > row_stride and not any(n > 1 and step == row_stride for n, step in zip(t.shape, t.stride())):
+            raise ValueError(f"rows of a contiguous tensor {tuple(t.shape)} do not lie {row_stride} entries apart")
         return _ptr(t)
     inner = 1
     for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):

@@ -100,3 +100,23 @@ def test_a_block_loop_over_prefixes_of_both_types_is_refused_before_anything_hap
         step_fn if callback else None, None, None)
     assert status == fdd.FDD_ERR_STATE
     assert host.fake_launches() == launched and not called
+
+
+@pytest.mark.parametrize("shape,pitch,fits", [
+    ((6, 2, 64), 128, True), ((6, 2, 64), 384, False), ((6, 2, 64), 256, False),     # rows as they lie, and as they do not
+    ((1, 2, 64), 384, True),                                                         # one row has no pitch
+    ((2, 3, 2, 64), 128, True), ((2, 3, 2, 64), 384, True), ((2, 3, 2, 64), 256, False),
+    ((1, 6, 2, 64), 384, False), ((6, 128), 128, True), ((768,), 384, False),
+])
+def test_the_stated_pitch_of_contiguous_rows_is_theirs(shape, pitch, fits):
+    import torch
+    t = torch.zeros(shape, dtype=torch.bfloat16)
+    if fits:
+        assert fdd._rows_ptr(t, pitch).value == t.data_ptr()
+        return
+    with pytest.raises(ValueError):
+        fdd._rows_ptr(t, pitch)
+    for call in (lambda: fdd.fdd_prefix_write(None, [], 0, t, t, [1], pitch, 0, stream=0),
+                 lambda: fdd.fdd_prefix_read(None, None, 0, 0, 1, t, t, pitch, stream=0)):
+        with pytest.raises(ValueError):
+            call()
