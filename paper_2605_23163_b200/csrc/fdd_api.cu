@@ -442,6 +442,8 @@ fdd_status commit_layers(fdd_ctx* ctx, fdd_forkset* const* sets, int n_sets, int
         if (st != FDD_OK) return st;
     }
     if (to_prefix && sets[0]->quantized) {
+        st = check_device(ctx);
+        if (st != FDD_OK) return st;
         for (int l = 0; l < n_layers; ++l) {
             st = check_distinct(ctx, sets, n_sets, first_layer + l, block_len);
             if (st != FDD_OK) return st;

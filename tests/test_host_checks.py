@@ -120,3 +120,24 @@ def test_the_stated_pitch_of_contiguous_rows_is_theirs(shape, pitch, fits):
                  lambda: fdd.fdd_prefix_read(None, None, 0, 0, 1, t, t, pitch, stream=0)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_calls_on_8_bit_prefixes_and_scores_want_the_contexts_device_to_be_current(host, ctx, buf):
+    fs = _quantized(ctx, buf)
+    rows = buf(8 * HKV * DIM * 2)
+    calls = (
+        lambda: fdd.fdd_prefix_write(ctx, [fs], 0, rows, rows, [8], HKV * DIM, 1, stream=0),
+        lambda: fdd.fdd_prefix_extend(ctx, [fs], 0, rows, rows, [8], 1, stream=0),
+        lambda: fdd.fdd_prefix_read(ctx, fs, 0, 0, 8, rows, rows, HKV * DIM, stream=0),
+        lambda: host.fdd_score_tokens(ctx, buf(VOCAB * 4), buf(4), None, 1, 0, buf(4), None, None, None, None),
+    )
+    host.fake_set_device(1)
+    launched = host.fake_launches()
+    for call in calls[:3]:
+        _refused(fdd.FDD_ERR_STATE, call)
+    assert calls[3]() == fdd.FDD_ERR_STATE
+    assert host.fake_launches() == launched and fdd.fdd_forkset_prefix_len(fs) == 64
+    host.fake_set_device(0)
+    for call in calls:
+        assert call() == fdd.FDD_OK
+    assert host.fake_launches() == launched + 4 and fdd.fdd_forkset_prefix_len(fs) == 80
