@@ -334,7 +334,7 @@ fdd_status fdd_kv_commit(fdd_ctx* ctx, fdd_forkset* const* sets, int n_sets, int
  * only, so fork sets that already read the same buffers with a shorter length are not disturbed.
  * (A prefix in 8 bits, see fdd_fork_quantized: the block is rounded as it is written, and if the prefix ends inside a group of
  * 64 tokens the rows of that group may be rounded again under a larger exponent; a fork set that reads the same buffers with a
- * shorter length sees them so, in stream order.  A set, or a contiguous cache, given twice in a call is FDD_ERR_STATE.)
+ * shorter length sees them so, in stream order.  Sets and arrays given twice in a call are refused as by fdd_prefix_write.)
  * FDD_ERR_STATE if a set has more than one rollout or has committed a private suffix;
  * FDD_ERR_CAPACITY if P + d_s exceeds prefix_capacity (nothing is launched).  A page table entry
  * outside [0, prefix_capacity) is not followed: the rows are dropped and the device status word
@@ -352,9 +352,9 @@ fdd_status fdd_prefix_extend(fdd_ctx* ctx, fdd_forkset* const* sets, int n_sets,
  *               a fused projection are written as they lie: pass the width of its rows.)
  *   advance     != 0: the sets' prefix lengths grow afterwards (pass it on the last layer).
  * k and v are 16-byte aligned and are not part of a cache that the call writes.  FDD_ERR_STATE for a set with a bf16 prefix, several
- * rollouts or a private suffix, or a set or contiguous cache given twice; FDD_ERR_CAPACITY beyond prefix_capacity.  A page table
- * entry outside [0, prefix_capacity) is not followed: the rows are dropped and the device status word gets FDD_ERR_INVALID_ARG.
- * Pages of one call are distinct.  FDD_ERR_STATE if the context's device is not the current one (fdd_prefix_read, fdd_score_tokens and
+ * rollouts or a private suffix, a set given twice, a set whose K and V (entries or exponents) are one array, or contiguous sets that
+ * share any such array; FDD_ERR_CAPACITY beyond prefix_capacity.  A page table entry outside [0, prefix_capacity) is not followed:
+ * the rows are dropped and the device status word gets FDD_ERR_INVALID_ARG.  Pages of one call are distinct.  FDD_ERR_STATE if the context's device is not the current one (fdd_prefix_read, fdd_score_tokens and
  * fdd_prefix_extend into 8 bits likewise).  Nothing is allocated, nothing synchronised.
  */
 fdd_status fdd_prefix_write(fdd_ctx* ctx, fdd_forkset* const* sets, int n_sets, int layer,

@@ -167,14 +167,26 @@ fdd_status check_extends(fdd_ctx* ctx, const fdd_forkset* fs, int s, long long t
     return FDD_OK;
 }
 
-// No set, and no contiguous cache, twice in a call that writes prefixes: groups would be written by two CTAs at a time.  (Sets of
-// a paged context may share a pool; their pages are the caller's to keep apart.)
+// Nothing twice among the arrays that a call writes, entries and exponents of K and V: groups would be written by two CTAs at a
+// time, and one could round old rows down after the other has.  Within a set K and V are apart in either layout; contiguous sets share
+// none of the four.  (Sets of a paged context may share a pool; their pages are the caller's to keep apart.)
 fdd_status check_distinct(fdd_ctx* ctx, fdd_forkset* const* sets, int n_sets, int layer, const int32_t* n_tokens) {
-    for (int s = 1; s < n_sets; ++s)
-        for (int t = 0; t < s; ++t)
-            if (n_tokens[s] > 0 && n_tokens[t] > 0 &&
-                (sets[s] == sets[t] || (ctx->cfg.page_tokens == 0 && sets[s]->prefix_k[layer] == sets[t]->prefix_k[layer])))
+    for (int s = 0; s < n_sets; ++s) {
+        if (n_tokens[s] == 0) continue;
+        const void* const k = sets[s]->prefix_k[layer];
+        const void* const v = sets[s]->prefix_v[layer];
+        const int8_t* const ek = sets[s]->exp_k[layer];
+        const int8_t* const ev = sets[s]->exp_v[layer];
+        if (k == v || ek == ev) return fail(ctx, FDD_ERR_STATE, "set %d: K and V are one array", s);
+        for (int t = 0; t < s; ++t) {
+            if (n_tokens[t] == 0) continue;
+            const fdd_forkset* o = sets[t];
+            const bool share = k == o->prefix_k[layer] || v == o->prefix_v[layer] || k == o->prefix_v[layer] || v == o->prefix_k[layer] ||
+                               ek == o->exp_k[layer] || ev == o->exp_v[layer] || ek == o->exp_v[layer] || ev == o->exp_k[layer];
+            if (o == sets[s] || (ctx->cfg.page_tokens == 0 && share))
                 return fail(ctx, FDD_ERR_STATE, "sets %d and %d of the call are one set or share a cache", t, s);
+        }
+    }
     return FDD_OK;
 }
 

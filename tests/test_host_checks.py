@@ -141,3 +141,51 @@ def test_calls_on_8_bit_prefixes_and_scores_want_the_contexts_device_to_be_curre
     for call in calls:
         assert call() == fdd.FDD_OK
     assert host.fake_launches() == launched + 4 and fdd.fdd_forkset_prefix_len(fs) == 80
+
+
+@pytest.mark.parametrize("shared", ["k", "v", "ek", "ev", "k of one, v of the other", "ek of one, ev of the other"])
+def test_sets_that_share_any_array_of_a_contiguous_cache_are_not_written_in_one_call(host, ctx, buf, shared):
+    arrays = [dict(k=buf(HKV * CAP * DIM), v=buf(HKV * CAP * DIM), ek=buf(HKV * GROUPS), ev=buf(HKV * GROUPS)) for _ in range(2)]
+    if " of one" in shared:
+        arrays[1][shared.split(", ")[1].split()[0]] = arrays[0][shared.split()[0]]
+    else:
+        arrays[1][shared] = arrays[0][shared]
+    sets = [_quantized(ctx, buf, **a) for a in arrays]
+    rows = buf(16 * HKV * DIM * 2)
+    launched = host.fake_launches()
+    _refused(fdd.FDD_ERR_STATE, fdd.fdd_prefix_write, ctx, sets, 0, rows, rows, [8, 8], HKV * DIM, 1, stream=0)
+    _refused(fdd.FDD_ERR_STATE, fdd.fdd_prefix_extend, ctx, sets, 0, rows, rows, [8, 8], 1, stream=0)
+    assert host.fake_launches() == launched
+    fdd.fdd_prefix_write(ctx, sets, 0, rows, rows, [8, 0], HKV * DIM, 1, stream=0)       # one of them alone
+    assert host.fake_launches() == launched + 1
+
+
+@pytest.mark.parametrize("page", [0, 64])
+@pytest.mark.parametrize("shared", [("k", "v"), ("ek", "ev")])
+def test_a_set_whose_k_and_v_are_one_array_is_not_written(host, buf, page, shared):
+    c = fdd.fdd_create(HQ, HKV, DIM, VOCAB, 1, page, BLOCK, 8, fdd.FDD_LOGITS_F32)
+    try:
+        a = dict(k=buf(HKV * CAP * DIM), v=buf(HKV * CAP * DIM), ek=buf(HKV * GROUPS), ev=buf(HKV * GROUPS))
+        a[shared[1]] = a[shared[0]]
+        table = buf(4 * GROUPS) if page else None
+        fs = fdd.fdd_fork_quantized(c, [a["k"]], [a["v"]], [a["ek"]], [a["ev"]], table, 64, GROUPS if page else CAP, 1, [0], [None], [None], 0)
+        rows = buf(8 * HKV * DIM * 2)
+        launched = host.fake_launches()
+        _refused(fdd.FDD_ERR_STATE, fdd.fdd_prefix_write, c, [fs], 0, rows, rows, [8], HKV * DIM, 1, stream=0)
+        _refused(fdd.FDD_ERR_STATE, fdd.fdd_prefix_extend, c, [fs], 0, rows, rows, [8], 1, stream=0)
+        assert host.fake_launches() == launched
+        fdd.fdd_prefix_read(c, fs, 0, 0, 8, rows, rows, HKV * DIM, stream=0)             # reading is no matter
+    finally:
+        fdd.fdd_destroy(c)
+
+
+def test_paged_sets_may_share_a_pool(host, buf):
+    c = fdd.fdd_create(HQ, HKV, DIM, VOCAB, 1, 64, BLOCK, 8, fdd.FDD_LOGITS_F32)
+    try:
+        k, v, ek, ev = buf(HKV * CAP * DIM), buf(HKV * CAP * DIM), buf(HKV * GROUPS), buf(HKV * GROUPS)
+        sets = [fdd.fdd_fork_quantized(c, [k], [v], [ek], [ev], buf(4 * GROUPS), 64, GROUPS, 1, [0], [None], [None], 0) for _ in range(2)]
+        rows = buf(16 * HKV * DIM * 2)
+        fdd.fdd_prefix_write(c, sets, 0, rows, rows, [8, 8], HKV * DIM, 1, stream=0)
+        assert [fdd.fdd_forkset_prefix_len(fs) for fs in sets] == [72, 72]
+    finally:
+        fdd.fdd_destroy(c)
