@@ -107,7 +107,7 @@ uint64_t fdd_launch_count(const fdd_ctx* ctx);
  *   page_table          device int32 [ceil(prefix_len / page_tokens)] physical page of each
  *                       logical page (paged layout), NULL for the contiguous layout.  Every
  *                       entry must be in [0, prefix_capacity); entries are read on the device.
- *   prefix_len          valid prefix tokens (>= 0).
+ *   prefix_len          valid prefix tokens (>= 0, and at most 2^31 - 128, however the prefix grows: FDD_ERR_CAPACITY).
  *   prefix_capacity     tokens per head (contiguous) or number of physical pages (paged).
  *   n_forks             N >= 1, <= cfg.max_forks.
  *   seeds               host uint64 [N]: the noise key of each rollout (copied; the first call

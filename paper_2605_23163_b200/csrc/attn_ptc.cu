@@ -220,7 +220,7 @@ __device__ __forceinline__ int locate_group(const SetParams& p, int group) {
 }
 // The exponent there of K (which = 0) or V for KV head h; 0 for no group, or a page that is none of the pool's.
 __device__ __forceinline__ int load_exponent(const SetParams& p, const RawSet& r, int which, int place, int h) {
-    const int per_head = p.page_tokens != 0 ? p.n_phys_pages : (r.prefix_capacity + kKvGroup - 1) / kKvGroup;
+    const int per_head = p.page_tokens != 0 ? p.n_phys_pages : kv_groups(r.prefix_capacity);
     if (place < 0 || place >= per_head) return 0;
     const long long at = p.page_tokens != 0 ? static_cast<long long>(place) * p.n_kv_heads + h : static_cast<long long>(h) * per_head + place;
     return __ldg((which == 0 ? r.exp_k : r.exp_v) + at);

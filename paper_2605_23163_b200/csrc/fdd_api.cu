@@ -106,7 +106,7 @@ size_t prefix_cache_bytes(const fdd_config& c, const fdd_forkset* fs) {
 }
 // Groups of tokens that one head of a layer's prefix cache has room for, and the exponents of all of them.
 int cache_groups(const fdd_config& c, const fdd_forkset* fs) {
-    return c.page_tokens > 0 ? fs->prefix_capacity : (fs->prefix_capacity + kKvGroup - 1) / kKvGroup;
+    return c.page_tokens > 0 ? fs->prefix_capacity : kv_groups(fs->prefix_capacity);
 }
 size_t exponent_bytes(const fdd_config& c, const fdd_forkset* fs) {
     return fs->quantized ? static_cast<size_t>(cache_groups(c, fs)) * c.n_kv_heads : 0;
@@ -158,7 +158,7 @@ fdd_status check_extends(fdd_ctx* ctx, const fdd_forkset* fs, int s, long long t
         return fail(ctx, FDD_ERR_STATE, "set %d has a private suffix of %d tokens: the prefix must stay in front of it", s, fs->suffix_len);
     const int pt = ctx->cfg.page_tokens;
     const long long need = fs->prefix_len + tokens;
-    const bool fits = need <= 0x7FFFFFFF && (pt == 0 ? need <= fs->prefix_capacity : (need + pt - 1) / pt <= fs->prefix_capacity);
+    const bool fits = need <= kMaxPrefix && (pt == 0 ? need <= fs->prefix_capacity : (need + pt - 1) / pt <= fs->prefix_capacity);
     if (!fits)
         return fail(ctx, FDD_ERR_CAPACITY, "set %d: prefix %d + %s %lld exceeds the cache (%d %s)", s, fs->prefix_len, what,
                     tokens, fs->prefix_capacity, pt ? "pages" : "tokens");
@@ -652,6 +652,7 @@ static fdd_status fork_from(fdd_ctx* ctx, const void* const* prefix_k, const voi
         return fail(ctx, FDD_ERR_INVALID_ARG, "negative length or capacity");
     if (n_forks < 1 || n_forks > ctx->cfg.max_forks)
         return fail(ctx, FDD_ERR_CAPACITY, "n_forks = %d outside [1, %d]", n_forks, ctx->cfg.max_forks);
+    if (prefix_len > kMaxPrefix) return fail(ctx, FDD_ERR_CAPACITY, "prefix_len %d exceeds %d", prefix_len, kMaxPrefix);
     const int pt = ctx->cfg.page_tokens;
     if (pt == 0) {
         if (page_table) return fail(ctx, FDD_ERR_INVALID_ARG, "page_table given but the context is configured contiguous");

@@ -112,6 +112,9 @@ struct fdd_forkset {
     std::vector<int8_t*> exp_k, exp_v;      // per layer (empty for bf16)
 };
 constexpr int kKvGroup = 64;                // tokens that share an exponent: a page
+constexpr int kMaxPrefix = 0x7FFFFFFF - 127;   // tokens of a prefix: counts of pages and of 128-key tiles are rounded up in 32 bits
+// Groups of a head in a contiguous cache for so many tokens.  (A capacity may be any int.)
+__host__ __device__ inline int kv_groups(int tokens) { return static_cast<int>((static_cast<uint32_t>(tokens) + (kKvGroup - 1)) / kKvGroup); }
 
 // One scene's slice of a batched call, as the kernels see it.
 struct AttnProblem {

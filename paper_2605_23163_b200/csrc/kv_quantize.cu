@@ -51,7 +51,7 @@ __global__ void __launch_bounds__(kQuantThreads) quantize_kernel(const __grid_co
     uint8_t* const dst = qs.dst[which] + (qs.page_table != nullptr ? (slot * a.n_kv_heads + h) * kKvGroup
                                                                    : static_cast<long long>(h) * qs.cap + slot * kKvGroup) * D;
     int8_t* const exp_at = qs.exps[which] + (qs.page_table != nullptr ? slot * a.n_kv_heads + h
-                                                                      : h * static_cast<long long>((qs.cap + kKvGroup - 1) / kKvGroup) + slot);
+                                                                      : h * static_cast<long long>(kv_groups(qs.cap)) + slot);
     // rows [lo, hi_row) of the group are new, those in front of them are there already
     const int lo = max(0, qs.first - g * kKvGroup), hi_row = min(kKvGroup, qs.first + qs.count - g * kKvGroup);
     const __nv_bfloat16* const src = qs.src[which] + (static_cast<long long>(g) * kKvGroup - qs.first) * a.row_stride + static_cast<long long>(h) * D;
@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(kReadThreads) dequantize_kernel(const __grid_c
     tc::grid_dependency_wait();
     const uint32_t per_token = static_cast<uint32_t>(a.n_kv_heads) * kPerRow;
     const long long per_cache = static_cast<long long>(a.count) * per_token, runs = (per_cache + kRun - 1) / kRun;
-    const int groups = (a.cap + kKvGroup - 1) / kKvGroup;
+    const int groups = kv_groups(a.cap);
     for (long long run = blockIdx.x; run < 2 * runs; run += gridDim.x) {
         const int which = run >= runs ? 1 : 0;
         const long long begin = (run - which * runs) * kRun, row0 = begin / per_token;

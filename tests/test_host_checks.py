@@ -189,3 +189,36 @@ def test_paged_sets_may_share_a_pool(host, buf):
         assert [fdd.fdd_forkset_prefix_len(fs) for fs in sets] == [72, 72]
     finally:
         fdd.fdd_destroy(c)
+
+
+MOST = 2 ** 31 - 128             # tokens of a prefix
+
+
+def test_prefixes_end_where_their_tiles_can_still_be_counted(host, buf):
+    for page in (0, 64):
+        c = fdd.fdd_create(HQ, 1, DIM, VOCAB, 1, page, BLOCK, 8, fdd.FDD_LOGITS_F32)
+        try:
+            k, v, ek, ev, table, rows = (buf(4096) for _ in range(6))
+            caps = [2 ** 25, 2 ** 31 - 1] if page else [2 ** 31 - 1]
+
+            def fork8(length, cap):
+                return fdd.fdd_fork_quantized(c, [k], [v], [ek], [ev], table if page else None, length, cap, 1, [0], [None], [None], 0)
+
+            def fork16(length, cap):
+                return fdd.fdd_fork(c, [k], [v], table if page else None, length, cap, 1, [0], [None], [None], 0)
+
+            for fork in (fork8, fork16):
+                for cap in caps + [4]:
+                    for length in (MOST + 1, 2 ** 31 - 64, 2 ** 31 - 1):
+                        _refused(fdd.FDD_ERR_CAPACITY, fork, length, cap)
+                for cap in caps:
+                    fs = fork(MOST - 8, cap)
+                    launched = host.fake_launches()
+                    _refused(fdd.FDD_ERR_CAPACITY, fdd.fdd_prefix_extend, c, [fs], 0, rows, rows, [9], 1, stream=0)
+                    if fork is fork8:
+                        _refused(fdd.FDD_ERR_CAPACITY, fdd.fdd_prefix_write, c, [fs], 0, rows, rows, [9], DIM, 1, stream=0)
+                    assert host.fake_launches() == launched
+                    fdd.fdd_prefix_extend(c, [fs], 0, rows, rows, [8], 1, stream=0)
+                    assert fdd.fdd_forkset_prefix_len(fs) == MOST and host.fake_launches() == launched + 1
+        finally:
+            fdd.fdd_destroy(c)
