@@ -216,14 +216,14 @@ __device__ __forceinline__ TileTurn tile_turn(int i, int n) {
 // Where the exponents of a group of tokens lie: its page, or its place in a contiguous cache; -1 for a group beyond the prefix.
 __device__ __forceinline__ int locate_group(const SetParams& p, int group) {
     if (group >= (p.prefix_len + kKvGroup - 1) / kKvGroup) return -1;
-    return p.page_tokens != 0 ? __ldg(p.page_table + group) : group;
+    return p.page_tokens != 0 ? __ldcg(p.page_table + group) : group;
 }
 // The exponent there of K (which = 0) or V for KV head h; 0 for no group, or a page that is none of the pool's.
 __device__ __forceinline__ int load_exponent(const SetParams& p, const RawSet& r, int which, int place, int h) {
     const int per_head = p.page_tokens != 0 ? p.n_phys_pages : kv_groups(r.prefix_capacity);
     if (place < 0 || place >= per_head) return 0;
     const long long at = p.page_tokens != 0 ? static_cast<long long>(place) * p.n_kv_heads + h : static_cast<long long>(h) * per_head + place;
-    return __ldg((which == 0 ? r.exp_k : r.exp_v) + at);
+    return __ldcg((which == 0 ? r.exp_k : r.exp_v) + at);
 }
 
 // 32 rows of bytes ([rows][D], as TMA left them) as rows of a bf16 tile in the layout of its TMA copies ([chunk of 64 columns][128
@@ -940,7 +940,7 @@ attn_ptc_kernel(const __grid_constant__ TcArgs<MAXSETS> a) {
 #pragma unroll
                             for (int rh = 0; rh < 2; ++rh) {
                                 const int lp = t.index * 2 + rh;
-                                pages[rh] = lp < n_pages ? __ldg(p.page_table + lp) : p.n_phys_pages;
+                                pages[rh] = lp < n_pages ? __ldcg(p.page_table + lp) : p.n_phys_pages;
                             }
                         }
                         ok = tc::mbar_wait(tc::smem_u32(&bar_k_empty[s]), ph ^ 1, abort_flag, kWaitLimit);

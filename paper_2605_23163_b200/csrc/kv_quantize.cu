@@ -13,6 +13,8 @@
 // Bound by memory: 2 bytes read and 1 written per entry, and nothing to reuse.  One CTA takes a group (64 rows x D = 16 KB of
 // bf16 at D = 128) into registers, 8 entries a piece (16 bytes in, 8 out: neighbouring lanes read and write side by side) and 8 pieces
 // a thread, so that the maximum and the rounding need one read; the CTAs of a token's heads follow one another, since their rows lie side by side in the source.
+// No load goes through the read-only path: these kernels start while the one ahead may still write.  Rows and bytes, which nobody
+// reads twice, go past L1 (__ldcg).
 #include "fdd_internal.h"
 #include "tc_ptx.cuh"
 #include "e4m3.cuh"
@@ -62,7 +64,7 @@ __global__ void __launch_bounds__(kQuantThreads) quantize_kernel(const __grid_co
     for (int i = 0; i < kPieces; ++i) {
         const int piece = i * kQuantThreads + threadIdx.x, row = piece / kPerRow, c = piece % kPerRow;
         x[i] = make_uint4(0, 0, 0, 0);
-        if (row >= lo && row < hi_row) x[i] = __ldg(reinterpret_cast<const uint4*>(src + row * a.row_stride + c * 8));
+        if (row >= lo && row < hi_row) x[i] = __ldcg(reinterpret_cast<const uint4*>(src + row * a.row_stride + c * 8));
     }
 #pragma unroll
     for (int i = 0; i < kPieces; ++i)
@@ -143,7 +145,7 @@ __global__ void __launch_bounds__(kReadThreads) dequantize_kernel(const __grid_c
             const int token = a.first + static_cast<int>(row);
             long long entry, group;
             if (a.page_table != nullptr) {
-                const long long page = __ldg(a.page_table + token / kKvGroup);
+                const long long page = a.page_table[token / kKvGroup];
                 if (page < 0 || page >= a.cap) {         // not followed: the row is left as it is
                     atomicCAS(a.status, 0, FDD_ERR_INVALID_ARG);
                     continue;
@@ -154,8 +156,8 @@ __global__ void __launch_bounds__(kReadThreads) dequantize_kernel(const __grid_c
                 group = static_cast<long long>(h) * groups + token / kKvGroup;
                 entry = static_cast<long long>(h) * a.cap + token;
             }
-            q[i] = __ldg(reinterpret_cast<const uint2*>(a.src[which] + entry * D) + c);
-            e[i] = __ldg(a.exps[which] + group);
+            q[i] = __ldcg(reinterpret_cast<const uint2*>(a.src[which] + entry * D) + c);
+            e[i] = a.exps[which][group];                 // (out of L1: 64 tokens' pieces want it)
             to[i] = a.dst[which] + row * a.row_stride + static_cast<long long>(h) * D + c * 8;
         }
 #pragma unroll

@@ -46,3 +46,15 @@ def test_tensor_memory_is_taken_behind_the_wait_for_the_kernel_ahead():
             seen += 1
             assert "grid_dependency_wait()" in code[:code.index("tc::tmem_alloc(")], path
     assert seen == 1
+
+
+def test_kernels_that_start_early_read_nothing_as_read_only():
+    # The read-only path is for data that nobody writes while the kernel lives, and such a kernel's life overlaps that of the one
+    # whose results it waits for.  (It may also be moved ahead of the wait.)  What it would read wrongly depends on timing, so the
+    # code is read here.
+    seen = 0
+    for path in build.sources() + [h for h in build._headers() if h.endswith(".cuh")]:
+        code = re.sub(r"//[^\n]*", "", open(path).read())
+        seen += "grid_dependency_wait()" in code
+        assert "__ldg(" not in code and "ld.global.nc" not in code, path
+    assert seen >= 6
