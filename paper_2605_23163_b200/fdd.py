@@ -134,9 +134,10 @@ def _rows_ptr(t, row_stride):
         return _ptr(t)
     if t.is_contiguous():
         # (rows may be counted by several dimensions; what fits into one pitch is one row)
-        if t.numel() > row_stride and not any(n > 1 and step == row_stride for n, step in zip(t.shape, t.stride())):
+        if not (t.stride()[0] == row_stride and t.shape[0] > 1) and t.numel() > row_stride and \
+                not any(n > 1 and step == row_stride for n, step in zip(t.shape, t.stride())):
             raise ValueError(f"rows of a contiguous tensor {tuple(t.shape)} do not lie {row_stride} entries apart")
-        return _ptr(t)
+        return ctypes.c_void_p(t.data_ptr())
     inner = 1
     for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
         if size != 1 and stride != inner:

@@ -114,6 +114,10 @@ def test_the_stated_pitch_of_contiguous_rows_is_theirs(shape, pitch, fits):
     if fits:
         assert fdd._rows_ptr(t, pitch).value == t.data_ptr()
         return
+    beside = t.as_strided((1, *shape), (pitch, *t.stride()))       # (the stride of a dimension of one entry says nothing)
+    assert beside.is_contiguous()
+    with pytest.raises(ValueError):
+        fdd._rows_ptr(beside, pitch)
     with pytest.raises(ValueError):
         fdd._rows_ptr(t, pitch)
     for call in (lambda: fdd.fdd_prefix_write(None, [], 0, t, t, [1], pitch, 0, stream=0),
