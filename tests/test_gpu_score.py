@@ -183,3 +183,43 @@ def test_refusals():
         assert fdd.fdd_launch_count(ctx) == before
     finally:
         fdd.fdd_destroy(ctx)
+
+
+# Nearly certain rows.  With a peak `gap` nats above small logits that add up to S of it, the log-probability is -ln(1 + S) and the entropy
+# about S (1 + gap).  The 16 bytes around the peak are masked but for itself (inside them a sum is plain fp32), so every small term counts:
+# its t is off by 5 * 2^-24 of |t| <= 44 (difference, factor and constant, once in the pass and once where parts are moved), 9.1e-6 of the
+# term; the exponentials add 2^-21 and the sums of small terms, at most 75 + 20 additions, 95 * 2^-24 = 5.7e-6, the product with t and the
+# end 2^-21: 1.6e-5 in all.  A sum in one fp32 number would be off by 2^-24 of the peak a step, a tenth of S and more at 25 nats.
+CERTAIN_REL = 3e-5
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [1, 30, 100])                          # eight, two and one CTA a row at the larger vocabulary
+@pytest.mark.parametrize("vocab,gap", [(4096, 18.0), (151936, 18.0), (151936, 25.0), (151937, 29.5)])
+def test_rows_that_are_nearly_certain(rows, vocab, gap, dtype):
+    rng = np.random.default_rng(int(vocab + gap + rows))
+    per_piece = 8 if dtype == "bf16" else 4
+    logits = _round(rng.normal(size=(rows, vocab)) * 0.3, dtype)
+    peak = rng.integers(0, vocab, size=rows)
+    runner = np.empty(rows, dtype=np.int64)
+    for r in range(rows):
+        # the piece of a row begins at a multiple of 16 bytes of memory, the peak's is masked on both sides whatever that is
+        lo, hi = max(0, peak[r] - per_piece + 1), min(vocab, peak[r] + per_piece)
+        logits[r, lo:hi] = -np.inf
+        logits[r, peak[r]] = gap
+        # the likeliest of the rest: another piece of the same thread, a neighbour's, another CTA's
+        at = (peak[r] + (256 * per_piece, 2 * per_piece, vocab // 2)[r % 3]) % vocab
+        if lo <= at < hi:
+            at = (hi + 2 * per_piece) % vocab
+        runner[r] = at
+        logits[r, at] = _round(np.array(gap - 12.0), dtype)
+    tokens = np.where(np.arange(rows) % 4 == 3, runner, peak)
+    got = _score(logits, tokens, None, 2, dtype)
+    ref = score_tokens(logits, tokens, 2)
+    assert np.array_equal(got[2], ref["top_ids"])
+    assert np.all(got[0] <= 0.0) and np.all(got[1] >= 0.0) and np.all(got[3] <= 0.0)
+    sure = tokens == peak
+    assert np.all(np.abs(got[0][sure] - ref["logprob"][sure]) <= CERTAIN_REL * np.abs(ref["logprob"][sure]))
+    assert np.all(np.abs(got[3][:, 0] - ref["top_logprobs"][:, 0]) <= CERTAIN_REL * np.abs(ref["top_logprobs"][:, 0]))
+    assert np.all(np.abs(got[1] - ref["entropy"]) <= CERTAIN_REL * ref["entropy"])
+    assert np.all(np.abs(got[0] - ref["logprob"]) <= LOGPROB_ABS + REL * np.abs(ref["logprob"]))
