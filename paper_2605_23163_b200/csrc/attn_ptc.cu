@@ -79,8 +79,9 @@
 // same bf16 tiles as ever: an entry q * 2^E is a bf16 number, so nothing is lost on the way to the products, and neither the
 // soft-max nor the products know of the exponents.  TMA stages the groups of 64 tokens as bytes in a ring of their own, and a warpgroup more
 // (warps 12-15) turns them into the swizzled bf16 tiles that TMA writes otherwise; suffix and block come as before.  (e4m3
-// operands would double the rate of the products only with Q and P in 8 bits too.  Q could be two e4m3 numbers exactly, P could not: of
-// a row with one large weight and many small ones the small ones would be lost below 2^-18.)
+// operands would double the rate of the products only with Q and P in 8 bits too.  Two e4m3 numbers under one scale make up an entry
+// of Q exactly only where it is within about 2^10 of the largest, and a weight of P likewise: of a row with one large weight and many
+// small ones the small ones would lose bits below 2^-10 of it and be gone below 2^-18.)
 #include "fdd_internal.h"
 #include "tc_ptx.cuh"
 #include "tmap.h"
@@ -1999,8 +2000,8 @@ const int* resident_clusters(int device) {
 // 10 us more than the fit.  The fit is of launches with head dimension 128 on an otherwise idle chip; 64, and launches beside
 // the unmasking, go by the same.  Of two halves of the probabilities the query tiles' chains are serial: longer steps, and
 // four CTAs are never enough.  Prefixes in 8 bits have a fit of their own (16 / 2, 32 / 8, 4 / 1 and 28 / 4 heads, prefix 1000 to 12000, one to
-// eight rollouts): a step with one query tile turns as many bytes as one with two.  Before it had, in clusters / not: 16 / 2 heads, four
-// rollouts on 4003 tokens 27.1 / 24.7 us, two on 12000 29.6 / 24.7, 28 / 4 heads, one on 4003 29.3 / 24.7.
+// eight rollouts): a step with one query tile turns as many bytes as one with two.  By the other fit these went to clusters, and do not by this:
+// 16 / 2 heads, four rollouts on 4003 tokens 27.1 -> 24.8 us, two on 12000 29.6 -> 25.1, 28 / 4 heads, one on 4003 29.3 -> 25.1.
 bool unit_clusters(const SetParams& p, int ctas, const int* resident, int* size, int* unit) {
     if (p.tiles_total <= kWholeTiles) return false;
     struct Cost { int base, step; };
@@ -2152,6 +2153,8 @@ cudaError_t launch_attention_ptc(
     *n_launches += 1;
     // (32 KB of arguments cost a launch a microsecond or two: 28 / 4 heads, two layers 303 -> 298 us a block without them)
     if (n == 1) return launch_group<1>(ctx, probs, caches, n, head_dim, st, beside, alone);
+    // (not for prefixes in 8 bits: that kernel is made for one pair and for kTcMaxSets only, ten instantiations less to compile, and two
+    // to four pairs pay the microsecond: two scenes of four rollouts on 1000 tokens 25.1 us, over bf16 21.1)
     if (!kQuantized && n <= kTcFewSets) return launch_group<kQuantized ? kTcMaxSets : kTcFewSets>(ctx, probs, caches, n, head_dim, st, beside, alone);
     return launch_group<kTcMaxSets>(ctx, probs, caches, n, head_dim, st, beside, alone);
 }

@@ -476,9 +476,10 @@ cudaError_t launch_typed(const ScoreArgs& a, cudaStream_t st) {
 }  // namespace
 
 cudaError_t launch_score(ScoreArgs a, int logits_dtype, int sm_count, cudaStream_t st) {
-    // CTAs per row: as many as have an SM each, as long as every thread has pieces to look at.  (22 rows of 151936 with five alternatives, 1, 2, 4
-    // or 8 CTAs a row: 16.5, 13.3, 11.0, 11.9 us; 76 rows with 20: 19.7, 20.0, 22.3, 30.0; 152 rows: 28.2, 31.3, 29.9, 48.7.  What a CTA does
-    // besides its pass, 4 to 8 us, is done by each.)
+    // CTAs per row: as many as have an SM each, as long as every thread has pieces to look at.  (Rows of 151936 bf16 logits, 1, 2, 4 or
+    // 8 CTAs a row: 22 rows with five alternatives 18.5, 13.8, 11.0, 11.1 us; 40 rows with 20 21.4, 16.3, 15.1, 16.9; 76 rows 21.6, 18.3, 17.7,
+    // 27.0, without alternatives 16.7, 12.8, 12.4, 13.3; 152 rows with 20 24.7, 23.6, 28.8, 43.1; 300 rows 34.0, 38.1, 44.9, 73.7.  What a CTA
+    // does besides its pass, 4 to 8 us, is done by each.  Some 40 to 150 rows would gain 1 to 4 us by more CTAs than this rule has.)
     const int per_piece = logits_dtype == FDD_LOGITS_BF16 ? 8 : 4;
     a.cluster = 1;
     while (a.cluster < 8 && a.rows * a.cluster * 2 <= sm_count && a.vocab >= a.cluster * 2 * kScoreThreads * per_piece) a.cluster *= 2;
