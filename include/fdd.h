@@ -357,8 +357,9 @@ fdd_status fdd_prefix_extend(fdd_ctx* ctx, fdd_forkset* const* sets, int n_sets,
  * k and v are 16-byte aligned and are not part of a cache that the call writes.  FDD_ERR_STATE for a set with a bf16 prefix, several
  * rollouts or a private suffix, a set given twice, a set whose K and V (entries or exponents) are one array, or contiguous sets that
  * share any such array; FDD_ERR_CAPACITY beyond prefix_capacity.  A page table entry outside [0, prefix_capacity) is not followed:
- * the rows are dropped and the device status word gets FDD_ERR_INVALID_ARG.  Pages of one call are distinct.  FDD_ERR_STATE if the context's device is not the current one (fdd_prefix_read, fdd_score_tokens and
- * fdd_prefix_extend into 8 bits likewise).  Nothing is allocated, nothing synchronised.
+ * the rows are dropped and the device status word gets FDD_ERR_INVALID_ARG.  Pages of one call are distinct.  FDD_ERR_STATE if the
+ * context's device is not the current one (fdd_prefix_read, fdd_score_tokens and fdd_prefix_extend into 8 bits likewise).  Nothing is
+ * allocated, nothing synchronised.
  */
 fdd_status fdd_prefix_write(fdd_ctx* ctx, fdd_forkset* const* sets, int n_sets, int layer,
                             const void* k, const void* v, const int32_t* n_tokens, long long row_stride,
