@@ -60,7 +60,7 @@
 // large V, is done again in fp32 (redo_columns).  TMEM is S0 | S1 | O0 | O1 for them: each query tile has scores of its own, and
 // the two halves of P overwrite them.  The chain of a query tile (scores, soft-max, output, the next scores)
 // is then a serial one, one issuing warp each; the other tile's chain fills the gaps.  Three products of a
-// tile step instead of two are 3072 clocks of the tensor pipe, what a step of the other layout takes with
+// tile step instead of two are 3 x 1024 clocks of the tensor pipe, what a step of the other layout takes with
 // two (its soft-max groups are the limit), so nothing is gained by overlapping more.  Measured: a block of
 // six rollouts, 28 / 4 heads, 27 positions, prefix 3001, two layers: 6180 us with the CUDA-core kernel that
 // served these shapes (32 rows a CTA, fp32 FMA), 530 us with this.
